@@ -679,25 +679,27 @@ lse_kernel(const float2* __restrict__ partial, int64_t pitch, int tiles, TokenTa
 // are there twice, as dz has them.  Bound by memory: 18.4K rows of width 4096 47 us, 6.4 TB/s.
 template <typename T>
 __global__ void __launch_bounds__(256)
-gather_kernel(const T* __restrict__ hidden, T* __restrict__ rows, int pieces, int n_rows, int parts, TokenTables tab,
+gather_kernel(const T* __restrict__ hidden, T* __restrict__ rows, int pieces, int n_rows, int k_rows, int parts, TokenTables tab,
               const float* __restrict__ lse, const float* __restrict__ d_logp, float* __restrict__ lse_rows,
               float* __restrict__ coef, const int* gate, int want) {
   if (gate && *gate != want) return;
-  const int b = blockIdx.x, r = parts == 1 ? b : (b >> 5) * 16 + (b & 15);
-  const bool there = r < n_rows;
-  const int64_t t = there ? tab.row[r] : 0;
-  const float4* src = (const float4*)hidden + t * pieces;
-  float4* dst = (float4*)rows + (int64_t)b * pieces;
-  for (int i = threadIdx.x; i < pieces; i += 256) dst[i] = there ? src[i] : make_float4(0.f, 0.f, 0.f, 0.f);
-  if (lse_rows && (parts == 1 || !(b & 16)) && threadIdx.x < 64) {
-    float c = 0.f;
-    if (there)
-      for (int e = tab.edge_ptr[r] + (int)threadIdx.x; e < tab.edge_ptr[r + 1]; e += 64) c += d_logp[tab.edge_token[e]];
+  for (int b = blockIdx.x; b < k_rows; b += gridDim.x) {
+    const int r = parts == 1 ? b : (b >> 5) * 16 + (b & 15);
+    const bool there = r < n_rows;
+    const int64_t t = there ? tab.row[r] : 0;
+    const float4* src = (const float4*)hidden + t * pieces;
+    float4* dst = (float4*)rows + (int64_t)b * pieces;
+    for (int i = threadIdx.x; i < pieces; i += 256) dst[i] = there ? src[i] : make_float4(0.f, 0.f, 0.f, 0.f);
+    if (lse_rows && (parts == 1 || !(b & 16)) && threadIdx.x < 64) {
+      float c = 0.f;
+      if (there)
+        for (int e = tab.edge_ptr[r] + (int)threadIdx.x; e < tab.edge_ptr[r + 1]; e += 64) c += d_logp[tab.edge_token[e]];
 #pragma unroll
-    for (int s = 1; s < 64; s <<= 1) c += __shfl_xor(c, s);
-    if (threadIdx.x == 0) {
-      coef[r] = c;
-      lse_rows[r] = there ? lse[t] : 0.f;
+      for (int s = 1; s < 64; s <<= 1) c += __shfl_xor(c, s);
+      if (threadIdx.x == 0) {
+        coef[r] = c;
+        lse_rows[r] = there ? lse[t] : 0.f;
+      }
     }
   }
 }
@@ -707,43 +709,44 @@ gather_kernel(const T* __restrict__ hidden, T* __restrict__ rows, int pieces, in
 // or NaN (products of its planes would overflow, with either sign): the fp32 instruction then does the call.
 // Bound by memory: 36.6K rows of width 1024 in two launches 61 us for 375 MB.
 __global__ void __launch_bounds__(256)
-split_kernel(const float* __restrict__ src, const int32_t* __restrict__ row, int64_t n_rows, char* __restrict__ out, int64_t plane,
+split_kernel(const float* __restrict__ src, const int32_t* __restrict__ row, int n_rows, int out_rows, char* __restrict__ out, int64_t plane,
              int width, int* __restrict__ big, TokenTables tab, const float* __restrict__ lse, const float* __restrict__ d_logp,
              float scale, float* __restrict__ lse_rows, float* __restrict__ coef) {
-  const int64_t r = blockIdx.x;
-  const bool there = r < n_rows;
-  const int64_t t = there ? (row ? row[r] : r) : 0;
   bool beyond = false;
-  for (int i = threadIdx.x * 4; i < width; i += 1024) {
-    f32x4 x = {0.f, 0.f, 0.f, 0.f};
-    if (there) x = *(const f32x4*)(src + t * width + i);
+  for (int64_t r = blockIdx.x; r < out_rows; r += gridDim.x) {
+    const bool there = r < n_rows;
+    const int64_t t = there ? (row ? row[r] : r) : 0;
+    for (int i = threadIdx.x * 4; i < width; i += 1024) {
+      f32x4 x = {0.f, 0.f, 0.f, 0.f};
+      if (there) x = *(const f32x4*)(src + t * width + i);
 #pragma unroll
-    for (int v = 0; v < 4; ++v) beyond |= !(fabsf(x[v]) < 0x1p40f);
-    if (out)
+      for (int v = 0; v < 4; ++v) beyond |= !(fabsf(x[v]) < 0x1p40f);
+      if (out)
 #pragma unroll
-      for (int q = 0; q < 3; ++q) {
-        bf16x4 b;
+        for (int q = 0; q < 3; ++q) {
+          bf16x4 b;
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          b[v] = (__bf16)x[v];
-          x[v] -= (float)b[v];
+          for (int v = 0; v < 4; ++v) {
+            b[v] = (__bf16)x[v];
+            x[v] -= (float)b[v];
+          }
+          *(bf16x4*)(out + q * plane + (r * width + i) * 2) = b;
         }
-        *(bf16x4*)(out + q * plane + (r * width + i) * 2) = b;
-      }
-  }
-  if (coef && threadIdx.x < 64) {
-    float c = 0.f;
-    if (there)
-      for (int e = tab.edge_ptr[r] + (int)threadIdx.x; e < tab.edge_ptr[r + 1]; e += 64) {
-        c += d_logp[tab.edge_token[e]];
-        beyond |= !(fabsf(d_logp[tab.edge_token[e]] * scale) < 0x1p40f);
-      }
+    }
+    if (coef && threadIdx.x < 64) {
+      float c = 0.f;
+      if (there)
+        for (int e = tab.edge_ptr[r] + (int)threadIdx.x; e < tab.edge_ptr[r + 1]; e += 64) {
+          c += d_logp[tab.edge_token[e]];
+          beyond |= !(fabsf(d_logp[tab.edge_token[e]] * scale) < 0x1p40f);
+        }
 #pragma unroll
-    for (int s = 1; s < 64; s <<= 1) c += __shfl_xor(c, s);
-    beyond |= !(fabsf(c * scale) < 0x1p40f);
-    if (threadIdx.x == 0) {
-      coef[r] = c;
-      lse_rows[r] = there ? lse[t] : 0.f;
+      for (int s = 1; s < 64; s <<= 1) c += __shfl_xor(c, s);
+      beyond |= !(fabsf(c * scale) < 0x1p40f);
+      if (threadIdx.x == 0) {
+        coef[r] = c;
+        lse_rows[r] = there ? lse[t] : 0.f;
+      }
     }
   }
   if (beyond) *big = 1;
@@ -1190,6 +1193,8 @@ Plan plan_for(Kind kind, const dta_tokens* t, const dta_vocab_params_t* p, bool 
   s.k_rows = s.parts * ceil_div(s.R, 64) * 64;
   const int64_t groups = ceil_div(s.V, 256);   // of ids
   int64_t most = groups;
+  // a launch has fewer than 2^32 threads, and the form with the smallest tiles 16 logits a thread
+  most = std::min(most, std::max<int64_t>(1, ((int64_t)1 << 36) / s.padded / 256));
   // dz of a block takes up to 2 GiB, and so do the planes of its part of the matrix
   if (backward) most = std::min(most, std::max<int64_t>(1, ((int64_t)1 << 31) / (s.parts * s.padded * s.size * s.planes) / 256));
   if (kind == kParts) most = std::min(most, std::max<int64_t>(1, ((int64_t)1 << 31) / (6 * s.D) / 256));
@@ -1301,23 +1306,26 @@ LogitArgs logit_args(const VocabArgs& a, const Plan& s, int64_t v0, int64_t n, c
   return l;
 }
 
+// Blocks of a launch that has one for every row, of 256 threads each: fewer than 2^32 threads, the rest in further rounds.
+size_t row_blocks(int64_t rows) { return (size_t)std::min<int64_t>(rows, 1 << 23); }
+
 // Planes of the hidden rows; where the vocabulary comes in blocks, a look over the whole matrix, so that all of them are
 // multiplied the same way.
 void split_rows(const VocabArgs& a, const Plan& s, bool backward) {
   int* const big = (int*)(a.workspace + s.at_big);
   float* const none = nullptr;
   launch(a, false, clear_kernel, 1, 1, big);
-  launch(a, false, split_kernel, (size_t)s.k_rows, 256, (const float*)a.hidden, a.tab.row, s.R, a.workspace + s.at_planes_h,
+  launch(a, false, split_kernel, row_blocks(s.k_rows), 256, (const float*)a.hidden, a.tab.row, s.R, s.k_rows, a.workspace + s.at_planes_h,
          s.k_rows * s.D * 2, (int)s.D, big, a.tab, a.lse_in, a.d_logp, a.p.scale, backward ? (float*)(a.workspace + s.at_lse) : none,
          backward ? (float*)(a.workspace + s.at_coef) : none);
   if (s.blocks > 1)
-    launch(a, false, split_kernel, (size_t)s.V, 256, (const float*)a.weight, (const int32_t*)nullptr, s.V, (char*)nullptr, (int64_t)0,
+    launch(a, false, split_kernel, row_blocks(s.V), 256, (const float*)a.weight, (const int32_t*)nullptr, s.V, s.V, (char*)nullptr, (int64_t)0,
            (int)s.D, big, a.tab, (const float*)nullptr, (const float*)nullptr, 0.f, none, none);
 }
 // Planes of a block of the matrix.
 void split_matrix(const VocabArgs& a, const Plan& s, int64_t v0, int64_t n) {
   float* const none = nullptr;
-  launch(a, false, split_kernel, (size_t)n, 256, (const float*)a.weight + v0 * s.D, (const int32_t*)nullptr, n,
+  launch(a, false, split_kernel, row_blocks(n), 256, (const float*)a.weight + v0 * s.D, (const int32_t*)nullptr, n, n,
          a.workspace + s.at_planes_w, s.block * s.D * 2, (int)s.D, (int*)(a.workspace + s.at_big), a.tab, (const float*)nullptr,
          (const float*)nullptr, 0.f, none, none);
 }
@@ -1348,8 +1356,8 @@ void lse_of_rows(const VocabArgs& a, const Plan& s, const Gate& gate, bool last)
 // The rows themselves, gathered, for one-plane products; with lse and c (`sums`).
 template <typename T>
 void gather_rows(const VocabArgs& a, const Plan& s, const Gate& gate, bool sums) {
-  launch(a, false, gather_kernel<T>, (size_t)s.k_rows, 256, (const T*)a.hidden, (T*)(a.workspace + s.at_rows),
-         (int)(s.D * sizeof(T) / 16), (int)s.R, s.parts, a.tab, a.lse_in, a.d_logp, sums ? (float*)(a.workspace + s.at_lse) : nullptr,
+  launch(a, false, gather_kernel<T>, row_blocks(s.k_rows), 256, (const T*)a.hidden, (T*)(a.workspace + s.at_rows),
+         (int)(s.D * sizeof(T) / 16), s.R, s.k_rows, s.parts, a.tab, a.lse_in, a.d_logp, sums ? (float*)(a.workspace + s.at_lse) : nullptr,
          (float*)(a.workspace + s.at_coef), gate.flag, gate.want);
 }
 
@@ -1359,11 +1367,11 @@ int logprob_fwd(const VocabArgs& a) {
   clear_hip_error();
   if (a.p.dtype == DTA_BF16) {
     if (s.pack) gather_rows<__bf16>(a, s, Gate(), false);
-    if (s.R) fwd_block<Bf16>(a, s, 0, Gate());
+    for (int64_t b = 0; b < s.blocks; ++b) fwd_block<Bf16>(a, s, b, Gate());   // (none without rows)
     lse_of_rows<Bf16>(a, s, Gate(), true);
   } else if (s.kind != kParts) {
     if (s.pack) gather_rows<float>(a, s, Gate(), false);
-    if (s.R) fwd_block<F32>(a, s, 0, Gate());
+    for (int64_t b = 0; b < s.blocks; ++b) fwd_block<F32>(a, s, b, Gate());
     lse_of_rows<F32>(a, s, Gate(), true);
   } else {
     const Gate parts{(const int*)(a.workspace + s.at_big), 0}, big{parts.flag, 1};

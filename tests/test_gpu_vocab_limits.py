@@ -1,0 +1,43 @@
+"""GPU tests of the vocabulary ends at the limits of their sizes and lifetimes: calls of more logits than one launch has
+threads for, and token tables given back behind calls that have not run.  Bounds as in tests/test_gpu_vocab.py."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2602_00482_amd as dta
+
+pytestmark = pytest.mark.gpu
+
+U, UM = 2.0 ** -24, 2.0 ** -23
+TORCH = {"bf16": torch.bfloat16, "f32": torch.float32}
+KIND = {"bf16": dta.BF16, "f32": dta.F32}
+
+
+@pytest.mark.parametrize("dtype,rows,V", [("bf16", 2 ** 21, 2 ** 18 + 300), ("f32", 2 ** 20 + 3, 2 ** 18 + 300)])
+def test_more_logits_than_a_launch_has_threads_for(dtype, rows, V):
+    """2^39 logits (f32: 2^38) in launches over parts of the vocabulary: 600 rows, the first and the last among them,
+    against 64 bits."""
+    D = 64
+    rng = np.random.default_rng(rows)
+    ids = rng.integers(0, V, size=rows + 1).astype(np.int32)
+    ids[1], ids[-1] = 0, V - 1
+    tok = dta.tokens_build(dta.tree_build([-1], [rows + 1]), ids, V)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(7)
+    mk = lambda *s: torch.randn(s, generator=g, device="cuda").to(TORCH[dtype])
+    h, w = mk(rows + 1, D), mk(V, D) * (2 / math.sqrt(D))
+    logp, lse = dta.tree_logprob_fwd(tok, dta.VocabParams(D, 1.0, KIND[dtype]), h, w)
+    at = np.unique(np.concatenate(([0, rows - 1], rng.integers(0, rows, size=600))))
+    t = torch.from_numpy(at).cuda()
+    hd, wd = h[t].double(), w.double()
+    z = hd @ wd.t().contiguous()
+    ref = torch.logsumexp(z, 1)
+    want = z[torch.arange(len(at), device="cuda"), torch.from_numpy(ids[at + 1]).cuda().long()] - ref
+    zb = float((hd.abs() @ wd.abs().t().contiguous()).max()) * (D * UM + U)
+    lb = (128 + math.ceil(V / 128) / 64 + 12) * UM
+    assert ((lse[t].double() - ref).abs() <= zb + lb + 4 * U * ref.abs()).all()
+    assert ((logp[t + 1].double() - want).abs() <= 2 * zb + lb + 8 * U * (want.abs() + ref.abs())).all()
+    assert float(logp[0]) == 0 and float(lse[-1]) == 0
+    assert bool(torch.isfinite(lse).all()) and float(lse[:-1].min()) > math.log(V) - 1   # (every row was written)
