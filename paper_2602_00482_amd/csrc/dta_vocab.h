@@ -27,11 +27,14 @@ struct VocabArgs {
   // event the call's last launch may attach to itself, and whether it has; null: recorded afterwards
   hipEvent_t done_event;
   bool* done_recorded;
+  bool* failed;   // a launch of the call was refused: the rest of them are left out
 };
 
-// Launches a kernel on the call's stream; `last`: no launch of the call follows.
+// Launches a kernel on the call's stream; `last`: no launch of the call follows.  Nothing behind one that failed: it would read
+// what that one did not write.
 template <typename... P, typename... A>
 inline void launch(const VocabArgs& a, bool last, void (*kernel)(P...), size_t grid, unsigned block, A... args) {
+  if (*a.failed) return;
   if (last && a.done_event != nullptr) {
     hipExtLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(block), 0, a.stream, nullptr, a.done_event, 0,
                           static_cast<P>(args)...);
@@ -39,6 +42,7 @@ inline void launch(const VocabArgs& a, bool last, void (*kernel)(P...), size_t g
   } else {
     kernel<<<(unsigned)grid, block, 0, a.stream>>>(static_cast<P>(args)...);
   }
+  *a.failed = hipPeekAtLastError() != hipSuccess;
 }
 
 inline size_t elem_size(const dta_vocab_params_t& p) { return p.dtype == DTA_F32 ? 4 : 2; }

@@ -89,8 +89,9 @@ int run(dta_tokens* t, dta::VocabArgs& a, int (*launcher)(const dta::VocabArgs&)
     const int st = tables_on(t, dev, &a.tab);
     if (st != DTA_OK) return st;
     a.tokens = t;
-    bool recorded = false;
+    bool recorded = false, failed = false;
     a.done_recorded = &recorded;
+    a.failed = &failed;
     if (capture != hipStreamCaptureStatusNone) return launcher(a);
     const hipEvent_t ev = use_event(t, (void*)a.stream, dev);
     if (!ev) return DTA_ERR_HIP;

@@ -126,3 +126,37 @@ print(json.dumps([(call(tok, width, dtype, which), launches()) for which in ("em
 """, tokens if width > 64 else tokens // 8, width, dtype)   # (rows of 64: an eighth, for the host's memory)
     for status, all_ in got:
         assert status == 0 and len(all_) == 1 and all_[0][4] * all_[0][5] < 2 ** 32, all_
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_call_ends_at_a_launch_that_fails(recorded, dtype):
+    """Nothing is launched behind a launch that the runtime refuses, and the call says so."""
+    got = recorded("""
+dtype = dict(f32=dta.F32, bf16=dta.BF16)[sys.argv[2]]
+S = C.c_void_p(0x1000)
+ids = np.zeros(3001, dtype=np.int32)                      # (one id many times: sums in parts, two launches)
+build = lambda: dta.tokens_build(dta.tree_build([-1], [3001]), ids, 20000)
+out = []
+for which in ("embed_fwd", "embed_bwd", "logprob_fwd", "logprob_bwd"):
+    tok = build()
+    tok.prepare()
+    rec.rec_take()
+    assert call(tok, 512, dtype, which, S) == 0
+    n = len(launches())
+    rec.rec_finish(S)
+    tok.destroy()
+    for k in range(1, n + 1):
+        rec.rec_finish(S)
+        tok = build()
+        tok.prepare()
+        rec.rec_take()
+        rec.rec_fail(k)
+        status = call(tok, 512, dtype, which, S)
+        tried = launches()
+        tok.destroy()
+        out.append((which, n, k, status, [t[-1] for t in tried]))
+print(json.dumps(out))
+""", dtype)
+    assert {(w, n) for w, n, *_ in got} >= {("embed_fwd", 1), ("embed_bwd", 2)}
+    for which, n, k, status, tried in got:
+        assert status == -5 and tried == [1] * (k - 1) + [0], (which, n, k, status, tried)
