@@ -97,8 +97,8 @@ int run(dta_tokens* t, dta::VocabArgs& a, int (*launcher)(const dta::VocabArgs&)
     if (!ev) return DTA_ERR_HIP;
     a.done_event = ev;
     const int launched = launcher(a);
-    // (also after a launch that failed: those before it may be running)
-    if (!recorded && hipEventRecord(ev, a.stream) != hipSuccess) {
+    // (also after a launch that failed, which the event may have been attached to: those before it may be running)
+    if ((!recorded || launched != DTA_OK) && hipEventRecord(ev, a.stream) != hipSuccess) {
       (void)hipGetLastError();
       return launched != DTA_OK ? launched : DTA_ERR_HIP;
     }

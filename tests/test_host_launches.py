@@ -130,12 +130,16 @@ print(json.dumps([(call(tok, width, dtype, which), launches()) for which in ("em
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_a_call_ends_at_a_launch_that_fails(recorded, dtype):
-    """Nothing is launched behind a launch that the runtime refuses, and the call says so."""
+    """Nothing is launched behind a launch that the runtime refuses, the call says so, and the tables' memory is not given to
+    another upload before the launches in front of it have run."""
     got = recorded("""
 dtype = dict(f32=dta.F32, bf16=dta.BF16)[sys.argv[2]]
 S = C.c_void_p(0x1000)
 ids = np.zeros(3001, dtype=np.int32)                      # (one id many times: sums in parts, two launches)
 build = lambda: dta.tokens_build(dta.tree_build([-1], [3001]), ids, 20000)
+def upload(tok):
+    tok.prepare()
+    return [int(l.split()[1]) for l in rec.rec_take().decode().splitlines() if l.startswith("copy")][0]
 out = []
 for which in ("embed_fwd", "embed_bwd", "logprob_fwd", "logprob_bwd"):
     tok = build()
@@ -148,15 +152,22 @@ for which in ("embed_fwd", "embed_bwd", "logprob_fwd", "logprob_bwd"):
     for k in range(1, n + 1):
         rec.rec_finish(S)
         tok = build()
-        tok.prepare()
-        rec.rec_take()
+        block = upload(tok)
         rec.rec_fail(k)
         status = call(tok, 512, dtype, which, S)
         tried = launches()
         tok.destroy()
-        out.append((which, n, k, status, [t[-1] for t in tried]))
+        others, after = [build() for _ in range(40)], build()
+        while_running = block in [upload(o) for o in others]     # (all that is free is taken)
+        rec.rec_finish(S)
+        then = while_running or upload(after) == block
+        for o in others + [after]:
+            o.destroy()
+        out.append((which, n, k, status, [t[-1] for t in tried], while_running, then))
 print(json.dumps(out))
 """, dtype)
     assert {(w, n) for w, n, *_ in got} >= {("embed_fwd", 1), ("embed_bwd", 2)}
-    for which, n, k, status, tried in got:
+    for which, n, k, status, tried, while_running, then in got:
         assert status == -5 and tried == [1] * (k - 1) + [0], (which, n, k, status, tried)
+        # (a call whose first launch fails has left nothing that reads the tables)
+        assert then and while_running == (k == 1), (which, n, k)
