@@ -66,6 +66,7 @@ struct dta_tokens {
   // per stream that was used an event (hipEvent_t) that completes after the latest call on it
   struct Use {
     void* stream;
+    uint64_t thread;   // where the handle means another stream in every thread, the number of this one; 0 elsewhere
     int device;
     void* event;
   };

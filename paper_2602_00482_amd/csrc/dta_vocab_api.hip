@@ -1,4 +1,5 @@
 // C-ABI entry points of the vocabulary ends: argument checks, upload of the token tables, dispatch.  See include/dta.h.
+#include <atomic>
 #include <cstdio>
 #include <new>
 
@@ -37,11 +38,19 @@ int tables_on(dta_tokens* t, int dev, dta::TokenTables* out) {
   return DTA_OK;
 }
 
+// The calling thread's number, from 1 on; no other thread of the process has had it.
+uint64_t thread_number() {
+  static std::atomic<uint64_t> last{0};
+  static thread_local const uint64_t mine = ++last;
+  return mine;
+}
+
 // The event of the latest call on (stream, device).  Streams that are no longer used leave theirs behind;
 // completed ones are taken out when there are many.
 hipEvent_t use_event(dta_tokens* t, void* stream, int dev) {
+  const uint64_t thread = stream == (void*)hipStreamPerThread ? thread_number() : 0;
   for (const auto& u : t->uses)
-    if (u.stream == stream && u.device == dev) return (hipEvent_t)u.event;
+    if (u.stream == stream && u.thread == thread && u.device == dev) return (hipEvent_t)u.event;
   if (t->uses.size() >= 64) {
     size_t kept = 0;
     for (const auto& u : t->uses) {
@@ -61,7 +70,7 @@ hipEvent_t use_event(dta_tokens* t, void* stream, int dev) {
     (void)hipGetLastError();
     return nullptr;
   }
-  t->uses.push_back({stream, dev, ev});
+  t->uses.push_back({stream, thread, dev, ev});
   return ev;
 }
 

@@ -171,3 +171,42 @@ print(json.dumps(out))
         assert status == -5 and tried == [1] * (k - 1) + [0], (which, n, k, status, tried)
         # (a call whose first launch fails has left nothing that reads the tables)
         assert then and while_running == (k == 1), (which, n, k)
+
+
+@pytest.mark.parametrize("stream", [0, 2, 0x1000])
+def test_calls_of_two_threads_on_streams_of_one_handle(recorded, stream):
+    """hipStreamPerThread (2) is one handle and a stream of its own in every thread: the tables' memory is given to another
+    upload when the calls of both threads have run.  On a stream that the threads share the later call says it for both."""
+    got = recorded("""
+S = C.c_void_p(int(sys.argv[2]))
+build = lambda: chain(3000, 20000)
+def upload(tok):
+    tok.prepare()
+    return [int(l.split()[1]) for l in rec.rec_take().decode().splitlines() if l.startswith("copy")][0]
+tok = build()
+block = upload(tok)
+called, over, step = threading.Event(), threading.Event(), []
+def first():
+    step.append(call(tok, 64, dta.BF16, "embed_fwd", S))
+    called.set()
+    over.wait()
+    rec.rec_finish(S)
+def second():
+    step.append(call(tok, 64, dta.BF16, "embed_fwd", S))
+    rec.rec_finish(S)
+a = threading.Thread(target=first)
+a.start()
+called.wait()
+b = threading.Thread(target=second)
+b.start()
+b.join()
+tok.destroy()
+rec.rec_take()
+other, third = build(), build()
+one_ran = upload(other) == block
+over.set()
+a.join()
+both_ran = one_ran or upload(third) == block
+print(json.dumps([step, one_ran, both_ran]))
+""", stream)
+    assert got == [[0, 0], stream != 2, True]
