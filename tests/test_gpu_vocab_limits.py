@@ -41,3 +41,57 @@ def test_more_logits_than_a_launch_has_threads_for(dtype, rows, V):
     assert ((logp[t + 1].double() - want).abs() <= 2 * zb + lb + 8 * U * (want.abs() + ref.abs())).all()
     assert float(logp[0]) == 0 and float(lse[-1]) == 0
     assert bool(torch.isfinite(lse).all()) and float(lse[:-1].min()) > math.log(V) - 1   # (every row was written)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_tables_given_back_behind_calls_that_have_not_run(dtype):
+    """Calls on two streams behind long products; their tables are destroyed while both streams are still at the products, and
+    the memory of that size is then asked for until there is no more of it.  Uploads may share a hardware queue with one of the
+    streams and so wait for it: pairs of streams are tried until one pair is seen still at work behind the uploads."""
+    rows, V, D = 6000, 9000, 256
+    rng = np.random.default_rng(3)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    mk = lambda *s: torch.randn(s, generator=g, device="cuda").to(TORCH[dtype])
+    h, w, d_x, d = mk(rows, D), mk(V, D) * 0.1, mk(rows, D), torch.randn(rows, generator=g, device="cuda")
+    big = torch.randn(8192, 8192, device="cuda").bfloat16()
+    out = [torch.empty_like(big) for _ in range(2)]
+    p = dta.VocabParams(D, 1.0, KIND[dtype])
+    tree = dta.tree_build([-1, 0, 0], [rows // 2, rows // 4, rows // 4])
+    ids = rng.integers(0, V, size=rows).astype(np.int32)
+    build = lambda x: dta.tokens_build(tree, x, V)
+
+    def calls(tok):
+        x = dta.tree_embed_fwd(tok, p, w)
+        logp, lse = dta.tree_logprob_fwd(tok, p, h, w)
+        return (x, logp, lse, *dta.tree_logprob_bwd(tok, p, h, w, lse, d), dta.tree_embed_bwd(tok, p, d_x))
+
+    first = build(ids)
+    ref = calls(first)
+    torch.mm(big, big, out=out[0])
+    torch.cuda.synchronize()
+    overlapped = False
+    for attempt in range(6):
+        tok, streams = build(ids), [torch.cuda.Stream(), torch.cuda.Stream()]
+        tok.prepare()
+        others = [build(np.roll(ids, 1 + k)) for k in range(8)]
+        got, ends = [], []
+        for s, o in zip(streams, out):
+            with torch.cuda.stream(s):
+                for _ in range(40):                       # some 30 ms
+                    torch.mm(big, big, out=o)
+                got.append(calls(tok))
+                ends.append(torch.cuda.Event())
+                ends[-1].record(s)
+        tok.destroy()
+        assert not any(e.query() for e in ends), "the products were over before the tables were given back"
+        for o in others:
+            o.prepare()
+        overlapped = not any(e.query() for e in ends)
+        torch.cuda.synchronize()
+        for one in got:
+            for a, b in zip(ref, one):
+                assert torch.equal(a, b)
+        if overlapped:
+            break
+    assert overlapped
