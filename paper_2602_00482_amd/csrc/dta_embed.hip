@@ -47,12 +47,17 @@ struct Piece<__bf16> {
   }
 };
 
-// Results far larger than the memory-side cache (256 MB) are stored past it: they would drive out what the call still reads
-// and, dirty, be written out under the next call's reads.  us, by plain stores and past the cache, and the same with a
-// pass over the result behind it (width 2048, bf16): x of 64 MB 18 and 16, 41 and 47; 128 MB 33 and 31, 85 and 79; 256 MB 90 and 58,
-// 175 and 167; 512 MB 184 and 110, 338 and 318.  A table's gradient of 8192 tokens: 256 MB 61 and 56, 112 and 155; 512 MB 105 and
-// 106, 287 and 293; of 56462 tokens of width 4096 into 512 MB 243 and 203, 413 and 398, into 1 GB 336 and 310, 696 and 686.
-constexpr int64_t kStreamRows = (int64_t)128 << 20, kStreamTable = (int64_t)512 << 20;   // bytes of the result
+// Results that the memory-side cache (256 MB) cannot keep for the pass that reads them next are stored past it: they would drive
+// out what the call still reads and, dirty, be written out under the next pass' reads.  By itself a call is faster that way at
+// almost any size, but the pass behind it then finds nothing in the cache; what counts is both together.  us of both, by plain
+// stores and past the cache, and in brackets of the call alone (bf16, width 2560, three sets of tensors in turn; fp32 is alike):
+//   x of            112 MB 89, 94 (54, 31); 200 MB 150, 160 (91, 52); 300 MB 242, 232 (131, 76); 500 MB 391, 369 (208, 125)
+//   a table from 90 MB of d_x: 180 MB 120, 137 (72, 65); 250 MB 157, 176 (94, 80); 330 MB 216, 221 (113, 96);
+//                   420 MB 281, 268 (133, 113); 600 MB 380, 366 (170, 148); 1300 MB 753, 748 (291, 284)
+//   from 8 MB:      250 MB 131, 154; 330 MB 192, 197; 420 MB 245, 243; 850 MB 478, 479;  from 350 MB: 261, 266; 312, 313; 379, 369; 630, 602
+// The sign goes by the result's size, whatever d_x or the table beside it takes.  A table's pass behind begins while the call's
+// other reads still fill the cache: it crosses later.
+constexpr int64_t kStreamRows = (int64_t)256 << 20, kStreamTable = (int64_t)384 << 20;   // bytes of the result
 
 template <bool STREAM, typename R>   // (a type's choice: two branches are made one plain store)
 __device__ __forceinline__ void put_raw(R* p, const R& x) {
@@ -192,8 +197,9 @@ int embed_fwd(const VocabArgs& a) {
   const int rows = kThreads >> shift;
   const int64_t T_ = a.tokens->n_tokens;
   clear_hip_error();
-  launch(a, true, T_ * pieces * 16 >= kStreamRows ? embed_fwd_kernel<T, true> : embed_fwd_kernel<T, false>, (size_t)((T_ + rows - 1) / rows * cols), kThreads, (const T*)a.table, a.tab.id, (T*)a.x, T_,
-         pieces, shift, cols, a.p.scale);
+  const auto kernel = T_ * pieces * 16 >= kStreamRows ? embed_fwd_kernel<T, true> : embed_fwd_kernel<T, false>;
+  launch(a, true, kernel, (size_t)((T_ + rows - 1) / rows * cols), kThreads, (const T*)a.table, a.tab.id, (T*)a.x, T_, pieces, shift,
+         cols, a.p.scale);
   return launch_status("embeddings");
 }
 
@@ -206,8 +212,9 @@ int embed_bwd(const VocabArgs& a) {
   const int64_t zero_blocks = a.add || t->n_distinct == t->vocab ? 0 : ((int64_t)t->vocab + 31) / 32;
   float* partial = (float*)a.workspace;
   clear_hip_error();
-  launch(a, t->n_merges == 0, (int64_t)t->vocab * pieces * 16 >= kStreamTable ? embed_bwd_kernel<T, true> : embed_bwd_kernel<T, false>, (size_t)((part_blocks + zero_blocks) * cols), kThreads, (const T*)a.d_x, a.tab.part,
-         t->n_parts, a.tab.order, a.tab.present, t->vocab, a.d_table, partial, pieces, shift, cols, part_blocks, a.p.scale, a.add);
+  const auto kernel = (int64_t)t->vocab * pieces * 16 >= kStreamTable ? embed_bwd_kernel<T, true> : embed_bwd_kernel<T, false>;
+  launch(a, t->n_merges == 0, kernel, (size_t)((part_blocks + zero_blocks) * cols), kThreads, (const T*)a.d_x, a.tab.part, t->n_parts,
+         a.tab.order, a.tab.present, t->vocab, a.d_table, partial, pieces, shift, cols, part_blocks, a.p.scale, a.add);
   if (t->n_merges)
     launch(a, true, embed_merge_kernel<T>, (size_t)((t->n_merges + rows - 1) / rows * cols), kThreads, partial, a.tab.merge,
            t->n_merges, a.d_table, pieces, shift, cols, a.p.scale, a.add);

@@ -95,3 +95,29 @@ def test_tables_given_back_behind_calls_that_have_not_run(dtype):
         if overlapped:
             break
     assert overlapped
+
+
+@pytest.mark.parametrize("dtype,T,V,D", [("bf16", 67001, 97000, 2112), ("f32", 33001, 48000, 2112), ("bf16", 33001, 49001, 4160)])
+def test_embeddings_larger_than_the_memory_side_cache(dtype, T, V, D):
+    """x of 256 MiB and more and a table's gradient of 384 MiB and more, with long sums, are stored past the cache."""
+    size = torch.tensor([], dtype=TORCH[dtype]).element_size()
+    assert T * D * size >= 256 << 20 and V * D * size >= 384 << 20
+    rng = np.random.default_rng(5)
+    ids = rng.integers(0, V, size=T).astype(np.int32)
+    ids[rng.random(T) < 0.02] = V - 1
+    tok = dta.tokens_build(dta.tree_build([-1], [T]), ids, V)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    table, d_x = (torch.randn(n, D, generator=g, device="cuda").to(TORCH[dtype]) for n in (V, T))
+    p, at = dta.VocabParams(D, 1.25, KIND[dtype]), torch.from_numpy(ids).cuda().long()
+    x = dta.tree_embed_fwd(tok, p, table)
+    assert torch.equal(x, (table[at].float() * 1.25).to(TORCH[dtype]))   # (one product in fp32, one rounding)
+    d_table = dta.tree_embed_bwd(tok, p, d_x)
+    n = torch.bincount(at, minlength=V).double()[:, None]
+    ref = torch.zeros(V, D, device="cuda", dtype=torch.float64).index_add_(0, at, 1.25 * d_x.double())
+    sums = torch.zeros(V, D, device="cuda", dtype=torch.float64).index_add_(0, at, 1.25 * d_x.double().abs())
+    b = (n + 1) * U * sums
+    half = 2.0 ** -8 if dtype == "bf16" else U
+    over = (d_table.double() - ref).abs() - (b + half * (ref.abs() + b))
+    assert over.max().item() <= 0, over.max().item()
+    assert (d_table[n[:, 0] == 0] == 0).all()

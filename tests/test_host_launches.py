@@ -210,3 +210,24 @@ both_ran = one_ran or upload(third) == block
 print(json.dumps([step, one_ran, both_ran]))
 """, stream)
     assert got == [[0, 0], stream != 2, True]
+
+
+@pytest.mark.parametrize("dtype,size", [("bf16", 2), ("f32", 4)])
+def test_which_embeddings_are_stored_past_the_cache(recorded, dtype, size):
+    """Both sides of the measured crossings: results of 240 and 270 MiB of embeddings, 360 and 410 MiB of a table's gradient,
+    whatever the other tensor has; an accumulator is added to by plain stores."""
+    got = recorded("""
+dtype, size = dict(f32=dta.F32, bf16=dta.BF16)[sys.argv[2]], int(sys.argv[3])
+out = []
+def stream(which, T, vocab):
+    tok = chain(T, vocab)
+    assert call(tok, 1024, dtype, which) == 0
+    name = [l.split()[1] for l in rec.rec_take().decode().splitlines() if l.startswith("launch")][0]
+    return "Lb1" in name
+rows = lambda mib: mib * 1024 // size
+for other in (10, 10000, 300000):
+    out.append([stream("embed_fwd", rows(m), other) for m in (100, 240, 270, 900)])
+    out.append([stream("embed_bwd", other, rows(m)) for m in (200, 360, 410, 900)])
+print(json.dumps(out))
+""", dtype, size)
+    assert got == [[False, False, True, True]] * 6
