@@ -363,9 +363,11 @@ __device__ __forceinline__ void product(const Operand& A, const Operand& B, int6
       if (s < steps) walk.copy_step(lds_addr + s * F::kStageBytes);
     int stage = 0;
     for (int step = 0; step < steps; ++step) {
-      // this step's copies are in (those started after it may not be), and every wave has left the stage they go to next
+      // this step's copies are in (those started after it may not be), and every wave has left the stage they go to next: its
+      // reads of it have ended (as the compiler places the products they have anyway; here it does not rest on that)
       if (step + kAhead - 1 < steps) wait_copies<(kAhead - 1) * W::kCount>();
       else wait_copies<0>();
+      __builtin_amdgcn_s_waitcnt(0xC07F);
       block_barrier();
       if (step + kAhead < steps) walk.copy_step(lds_addr + (stage == 0 ? F::kStages - 1 : stage - 1) * F::kStageBytes);
       typename W::Lanes at;
