@@ -1142,7 +1142,10 @@ struct Choice {
   int form, splits;
   double time;
 };
+// (Numbers in parts do not take the narrowest form: they are for calls of many rows, and among 10^8 sizes of a forward call
+// and 4 10^6 of dH none would.)
 Choice choose(Kind kind, int64_t n, int64_t m, int64_t steps, bool may_split, int least = kFew) {
+  if (kind == kParts) least = std::max<int>(least, kThin);
   static const double step_us[2][kForms] = {{0.6, 0.65, 0.96, 1.05, 1.42}, {1.1, 2.1, 4.2, 4.2, 0}};
   static const double block_us[kForms] = {4, 4, 6, 6, 9}, read_tb[kForms] = {4.9, 4.9, 4.4, 3.0, 2.4};
   const int64_t pairs = kind == kParts ? 6 : 1;
@@ -1274,11 +1277,13 @@ Plan plan(const dta_tokens* t, const dta_vocab_params_t* p, bool backward, Plan*
 // Calls f(form) with the form's type.
 template <typename E, typename Fn>
 void with_form(int form, Fn f) {
-  if (form == kFew) f(Few());
-  else if (form == kThin) f(Thin());
-  else if (form == kWide) f(Wide());
-  else if (form == kMedium) f(Medium());
-  else if constexpr (sizeof(typename E::type) == 2) f(Large());
+  if constexpr (E::kPlanes == 1)
+    if (form == kFew) f(Few());
+  if (form == kThin) f(Thin());
+  if (form == kWide) f(Wide());
+  if (form == kMedium) f(Medium());
+  if constexpr (sizeof(typename E::type) == 2)
+    if (form == kLarge) f(Large());
 }
 
 // Whether a launch is meant, as the device finds out: *flag == want.

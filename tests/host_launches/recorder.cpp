@@ -69,6 +69,12 @@ const char* rec_take() {
   book.clear();
   return taken.c_str();
 }
+const char* rec_kernels() {   // all that the library has
+  std::lock_guard<std::mutex> lock(mu);
+  taken.clear();
+  for (const auto& k : kernels) taken += k.second + "\n";
+  return taken.c_str();
+}
 void rec_fail(int nth) { fail_in = nth; }
 void rec_capture(int on) { capturing = on; }
 void rec_finish(void* stream) {   // what the calling thread sees as that stream has run

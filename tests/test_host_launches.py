@@ -15,7 +15,7 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 PRELUDE = """
 import ctypes as C, json, re, sys, threading
 rec = C.CDLL(sys.argv[1], mode=C.RTLD_GLOBAL)
-rec.rec_take.restype = C.c_char_p
+rec.rec_take.restype = rec.rec_kernels.restype = C.c_char_p
 rec.rec_finish.argtypes = [C.c_void_p]
 import numpy as np
 import paper_2602_00482_amd as dta
@@ -231,3 +231,22 @@ for other in (10, 10000, 300000):
 print(json.dumps(out))
 """, dtype, size)
     assert got == [[False, False, True, True]] * 6
+
+
+def test_the_gpu_tests_reach_every_kernel_of_the_log_probabilities(recorded):
+    """The sizes of tests/test_gpu_vocab_forms.py take every kernel of dta_logprob.hip that the library has: no instance is
+    without a test, and none without a call."""
+    import test_gpu_vocab_forms as G
+    missing, every = recorded("""
+rec.rec_take()
+every = {n for n in rec.rec_kernels().decode().split() if re.search(r"(logits_fwd|logits_bwd|lse|gather|split|clear|grad|outer|sum)_kernel", n)}
+every = {n for n in every if "dta_f32" not in n and "attn" not in n}
+left = set(every)
+for dtype, rows, vocab, width in json.loads(sys.argv[2]):
+    tok = chain(rows + 1, vocab)
+    for which in ("logprob_fwd", "logprob_bwd"):
+        assert call(tok, width, dict(f32=dta.F32, bf16=dta.BF16)[dtype], which) == 0
+    left -= {l.split()[1] for l in rec.rec_take().decode().splitlines() if l.startswith("launch")}
+print(json.dumps([sorted(left), sorted(every)]))
+""", json.dumps(G.FORMS))
+    assert len(every) > 50 and missing == []
