@@ -1142,10 +1142,7 @@ struct Choice {
   int form, splits;
   double time;
 };
-// (Numbers in parts do not take the narrowest form: they are for calls of many rows, and among 10^8 sizes of a forward call
-// and 4 10^6 of dH none would.)
 Choice choose(Kind kind, int64_t n, int64_t m, int64_t steps, bool may_split, int least = kFew) {
-  if (kind == kParts) least = std::max<int>(least, kThin);
   static const double step_us[2][kForms] = {{0.6, 0.65, 0.96, 1.05, 1.42}, {1.1, 2.1, 4.2, 4.2, 0}};
   static const double block_us[kForms] = {4, 4, 6, 6, 9}, read_tb[kForms] = {4.9, 4.9, 4.4, 3.0, 2.4};
   const int64_t pairs = kind == kParts ? 6 : 1;
@@ -1183,6 +1180,11 @@ struct Plan {
   size_t at_big, at_lse, at_coef, at_rows, at_planes_h, at_planes_w, at_partial, at_dz, at_h, at_w, bytes;
 };
 
+// The narrowest form that the logits of a forward call and dH take: numbers in parts are for calls of many rows, and of 9 10^7
+// sizes of the one and 4 10^6 of the other none would take Few.  (The logits of a gradient do: 754 rows x 2529 x 5632 567 us,
+// and 626 on the fp32 instruction, which is next.)
+constexpr int least_form(int planes) { return planes == 3 ? kThin : kFew; }
+
 // block: 0, or what the blocks of the vocabulary have to be
 Plan plan_for(Kind kind, const dta_tokens* t, const dta_vocab_params_t* p, bool backward, int64_t block) {
   Plan s{};
@@ -1207,10 +1209,11 @@ Plan plan_for(Kind kind, const dta_tokens* t, const dta_vocab_params_t* p, bool 
   s.blocks = ceil_div(s.V, s.block);
   const int64_t width_steps = s.D * s.size / 128;
   const int64_t ids = s.blocks == 1 ? s.V : s.block;
-  s.z = choose(kind, backward ? ceil_div(s.R, 64) * 64 : s.R, ids, width_steps, false);   // (dz is padded to 64 rows)
+  const int least = least_form(s.planes);
+  s.z = choose(kind, backward ? ceil_div(s.R, 64) * 64 : s.R, ids, width_steps, false, backward ? kFew : least);   // (dz is padded to 64 rows)
   s.tiles = ceil_div(s.V, kTileM[s.z.form]);
   if (backward) {
-    s.h = choose(kind, s.parts * s.R, s.D, ceil_div(ids * s.size, 128), true);
+    s.h = choose(kind, s.parts * s.R, s.D, ceil_div(ids * s.size, 128), true, least);
     if (s.parts == 1) s.w = choose(kind, ids, s.D, s.k_rows * s.size / 128, true, kind == kF32 ? kThin : kWide);   // (dz by columns: rows of 256 bytes and more)
   }
   return s;
@@ -1274,10 +1277,10 @@ Plan plan(const dta_tokens* t, const dta_vocab_params_t* p, bool backward, Plan*
   return s;
 }
 
-// Calls f(form) with the form's type.
-template <typename E, typename Fn>
+// Calls f(form) with the form's type, LEAST or a wider one.
+template <typename E, int LEAST, typename Fn>
 void with_form(int form, Fn f) {
-  if constexpr (E::kPlanes == 1)
+  if constexpr (LEAST == kFew)
     if (form == kFew) f(Few());
   if (form == kThin) f(Thin());
   if (form == kWide) f(Wide());
@@ -1348,7 +1351,7 @@ void fwd_block(const VocabArgs& a, const Plan& s, int64_t b, const Gate& gate) {
   l.partial_pitch = s.tiles;
   l.first_tile = (int)(v0 / kTileM[s.z.form]);
   l.logp = a.logp;
-  with_form<E>(s.z.form, [&](auto f) {
+  with_form<E, least_form(E::kPlanes)>(s.z.form, [&](auto f) {
     typedef decltype(f) F;
     launch(a, false, logits_fwd_kernel<E, F>, (size_t)l.m_tiles * l.n_tiles, F::kThreads, l);
   });
@@ -1423,7 +1426,7 @@ void bwd_block(const VocabArgs& a, const Plan& s, int64_t b, const Gate& gate, b
   l.dz_pitch = s.block;
   l.dz_plane = dz_plane;
   l.dz_parts = planes ? 3 : s.parts;
-  with_form<E>(s.z.form, [&](auto f) {
+  with_form<E, kFew>(s.z.form, [&](auto f) {
     typedef decltype(f) F;
     launch(a, false, logits_bwd_kernel<E, F>, (size_t)l.m_tiles * l.n_tiles, F::kThreads, l, a.d_logp);
   });
@@ -1436,7 +1439,7 @@ void bwd_block(const VocabArgs& a, const Plan& s, int64_t b, const Gate& gate, b
     g.across = 4;
     g.gate = gate.flag;
     g.want = gate.want;
-    with_form<E>(c.form, [&](auto f) {
+    with_form<E, least_form(E::kPlanes)>(c.form, [&](auto f) {
       typedef decltype(f) F;
       if constexpr (!kWeight || F::BN * sizeof(typename E::type) >= 256)
         launch(a, last, grad_kernel<E, F, kWeight>, (size_t)g.m_tiles * g.n_tiles * g.splits, F::kThreads, g);

@@ -22,7 +22,7 @@ FORMS = [   # type, rows before a scored token, ids, width
     ("f32", 8, 40, 64), ("f32", 8, 33106, 64), ("f32", 809, 16881, 768), ("f32", 907, 16772, 192), ("f32", 1269, 195, 5440),
     ("f32", 1574, 2807, 832), ("f32", 8436, 1799, 192), ("f32", 17151, 129, 64), ("f32", 21772, 1817, 64),
     ("f32", 21778, 1382, 320), ("f32", 33871, 41, 64), ("f32", 41304, 928, 64),
-    ("f32", 3491, 4611, 35264),
+    ("f32", 3491, 4611, 35264), ("f32", 754, 2529, 5632),
 ]
 
 
