@@ -529,7 +529,12 @@ int dta_tree_embed_bwd(dta_tokens_t* tokens, const dta_vocab_params_t* params, c
  * In fp32 mode large calls multiply numbers in three bf16 parts each, all 24 bits; numbers
  * below 2^-110 are held to 2^-134.  Where a call has numbers from 2^40 on, infinities or
  * NaN the fp32 instruction does it, which the device finds out: the host does not wait.
- * The same holds for the backward call.  The workspace then takes up to 2 GiB of parts.
+ * The same holds for the backward call.
+ * The workspace holds, with R rows before a scored token (rounded up to 64):
+ *   8 bytes for each row and 128 ids;
+ *   fp32 in three parts: the parts of the rows, 6 R width bytes, and of as many ids as fit into 2 GiB, 256 at
+ *   least, 6 width bytes each;
+ *   hidden states of 4 GiB and more: the R rows.
  */
 int dta_tree_logprob_fwd(dta_tokens_t* tokens, const dta_vocab_params_t* params, const void* hidden,
                          const void* weight, float* logp, float* lse, void* workspace, size_t workspace_bytes,
@@ -549,10 +554,17 @@ int dta_tree_logprob_fwd(dta_tokens_t* tokens, const dta_vocab_params_t* params,
  *   d_weight : device [vocab, width] out, every row written, or, with DTA_GRAD_ADD in
  *              flags, an fp32 accumulator; or NULL: not wanted (not both NULL)
  * In bf16 mode dz is rounded to bf16 before the two products (its sums and theirs are
- * fp32); calls of at most 128 rows, where the products hide under the matrix' traffic,
- * keep 16 bits of it.
- * The workspace holds the rows, dz of as much of the vocabulary as fits into 2 GiB, and
- * partial sums.
+ * fp32), which moves a gradient by up to 2^-8 of the sum of its terms' magnitudes, also
+ * one that is added to an fp32 accumulator; calls of at most 128 rows, where the products
+ * hide under the matrix' traffic, keep 16 bits of it.
+ * The workspace holds (R rounded up to 256 here):
+ *   the R rows (bf16 calls of at most 128 rows: twice);
+ *   dz of as many ids as fit into 2 GiB, 256 at least: for each row and id 2 bytes in
+ *   bf16 (at most 128 rows: 4), 4 in fp32, 6 in fp32 in three parts;
+ *   sums of d_hidden, 4 R width bytes, and as much for every further split of a product
+ *   over the vocabulary (up to 64, where tiles alone would leave part of the chip idle);
+ *   of d_weight, where the product over the rows is split, 4 width bytes for each id of dz and split;
+ *   fp32 in three parts: their parts as in the forward call.
  */
 int dta_tree_logprob_bwd(dta_tokens_t* tokens, const dta_vocab_params_t* params, const void* hidden,
                          const void* weight, const float* lse, const float* d_logp, void* d_hidden,

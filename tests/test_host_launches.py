@@ -250,3 +250,39 @@ for dtype, rows, vocab, width in json.loads(sys.argv[2]):
 print(json.dumps([sorted(left), sorted(every)]))
 """, json.dumps(G.FORMS))
     assert len(every) > 50 and missing == []
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_workspaces_hold_what_the_header_says(recorded, dtype):
+    """The terms of the header on calls that are split, or not, into parts, and into blocks of the vocabulary."""
+    size = 4 if dtype == "f32" else 2
+    shapes = [(rows, vocab, width) for rows in (1, 100, 129, 3000, 50000, 1 << 20) for vocab in (500, 32000, 200003)
+              for width in (64, 1024, 4096)] + [(40000, 1000, 32768), (1 << 21, 3000, 4000 // 64 * 64)]
+    got = recorded("""
+dtype = dict(f32=dta.F32, bf16=dta.BF16)[sys.argv[2]]
+out = []
+toks = {}
+for rows, vocab, width in json.loads(sys.argv[3]):
+    if (rows, vocab) not in toks:
+        toks.clear()
+        toks[rows, vocab] = chain(rows + 1, vocab)
+    p = dta.VocabParams(width, 1.0, dtype)
+    out.append([dta.vocab_workspace_bytes(toks[rows, vocab], p, k) for k in (2, 3)])
+print(json.dumps(out))
+""", dtype, json.dumps(shapes))
+    up = lambda x, to: -(-x // to) * to
+    for (rows, vocab, width), (fwd, bwd) in zip(shapes, got):
+        R, T, GiB2 = up(rows, 64), rows + 1, 1 << 31
+        ids = min(up(vocab, 256), max(256, GiB2 // (6 * width)))
+        pairs, slack = 8 * rows * -(-vocab // 128), 8192
+        copied = R * width * size if T * width * size >= 1 << 32 else 0
+        plain, parts = pairs + copied + slack, pairs + copied + 6 * R * width + 6 * width * ids + slack
+        assert fwd <= (parts if dtype == "f32" else plain), (rows, vocab, width, fwd)
+        few = dtype == "bf16" and rows <= 128
+        R = up(rows, 256)
+        least = rows * width * size * (2 if few else 1) + 4 * rows * width          # the rows, one sum of d_hidden
+        dz = lambda b: R * b * min(up(vocab, 256), max(256, GiB2 // (R * b)))
+        each = (4 if few else 2) if dtype == "bf16" else 6
+        most = R * width * size * (2 if few else 1) + max(dz(each), dz(4)) + 64 * 4 * width * (R + min(up(vocab, 256), max(256, GiB2 // (2 * R)))) + \
+            (6 * R * width + 6 * width * ids if dtype == "f32" else 0) + 8 * R + slack
+        assert least <= bwd <= most, (rows, vocab, width, bwd, least, most)
