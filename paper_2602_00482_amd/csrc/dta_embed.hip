@@ -4,7 +4,7 @@
 // with id v: the host has sorted the tokens by id, so every row of the gradient has one owner that adds its tokens' rows
 // in ascending order in fp32: no atomics, and nothing is read or written twice but the partial sums of ids with more
 // than 64 tokens.  Both are bound by memory.  56462 tokens of width 4096, bf16: forward 141 us for the 0.93 GB that x and
-// its tokens' rows are (6.6 TB/s; rows of ids that come again are found in the caches); backward into 65536 rows 201 us, 12 of them
+// its tokens' rows are (6.6 TB/s; rows of ids that come again are found in the caches); backward into 65536 rows 201 us, 6 of them
 // for the long sums, for the 1.0 GB of d_x and d_table (5.0 TB/s; a large copy reaches 5.2).
 #include "dta_vocab.h"
 

@@ -8,11 +8,12 @@
 // the forward pass, and in the backward pass dz exists for a block of the vocabulary at a time.
 //
 // What bounds it: from about 200 rows on the matrix instructions, with fewer the way of W from memory.  Measured, bf16
-// unless said otherwise (rows x ids x width; a large library product of such sizes does 1.49 PFLOP/s, a large copy 5.2 TB/s):
-//   logits and their statistics   18.4K x 50021 x 2048 2.6 to 2.7 ms, 1.40 to 1.45 PFLOP/s; 18.4K x 65536 x 4096 6.61 ms, 1.49
-//   logits again and dz           the latter 6.84 ms;  dH 7.10 ms;  dW 7.14 ms: 1.44 to 1.38
+// unless said otherwise (rows x ids x width; a large library product of such sizes does 1.49 PFLOP/s, a large copy 5.2 TB/s; GPUs of
+// the kind differ by 5 % under the power limit):
+//   logits and their statistics   18.4K x 50021 x 2048 2.7 to 2.85 ms, 1.33 to 1.40 PFLOP/s; 18.4K x 65536 x 4096 6.6 to 7.0 ms, 1.42 to 1.49
+//   logits again and dz           the latter 6.8 to 7.1 ms;  dH 7.1 to 7.4 ms;  dW 7.1 to 7.5 ms: 1.45 to 1.32
 //   33 x 131072 x 4096            181 us, W at 5.9 TB/s
-//   fp32 in three parts           4.6K x 32000 x 1024 1.15 to 1.29 ms: 1.40 to 1.57 PFLOP/s of the bf16 instruction
+//   fp32 in three parts           4.6K x 32000 x 1024 1.2 to 1.36 ms: 1.33 to 1.50 PFLOP/s of the bf16 instruction
 #include <algorithm>
 #include <type_traits>
 
