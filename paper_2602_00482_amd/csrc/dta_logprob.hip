@@ -608,12 +608,15 @@ logits_fwd_kernel(LogitArgs a) {
     top = fmaxf(top, __shfl_xor(top, 32));
     float sum = 0.f;
     if (__builtin_amdgcn_ballot_w64(!(fabsf(top) < INFINITY))) {
-      // an infinite maximum: equal infinities count as exp 0, not exp NaN
+      // an infinite maximum: equal infinities count as exp 0, not exp NaN (added in the order of the other branch, so that the
+      // wave's other rows come out as without it)
 #pragma unroll
-      for (int i = 0; i < F::TM; ++i)
+      for (int i = 0; i < F::TM; ++i) {
+        float e[4];
 #pragma unroll
-        for (int v = 0; v < 4; ++v)
-          sum += __builtin_amdgcn_exp2f((acc[i][j][v] == top ? 0.f : acc[i][j][v] - top) * kExp2);
+        for (int v = 0; v < 4; ++v) e[v] = __builtin_amdgcn_exp2f((acc[i][j][v] == top ? 0.f : acc[i][j][v] - top) * kExp2);
+        sum += (e[0] + e[1]) + (e[2] + e[3]);
+      }
     } else {
 #pragma unroll
       for (int i = 0; i < F::TM; ++i) {   // (four exponentials, then their sum: an addition right behind its exponential waits)

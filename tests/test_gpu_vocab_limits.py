@@ -121,3 +121,37 @@ def test_embeddings_larger_than_the_memory_side_cache(dtype, T, V, D):
     over = (d_table.double() - ref).abs() - (b + half * (ref.abs() + b))
     assert over.max().item() <= 0, over.max().item()
     assert (d_table[n[:, 0] == 0] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,V,D", [(39, 300, 64), (300, 33000, 64), (1100, 16500, 64), (18700, 290, 320)])
+def test_infinite_logits_and_nan_stay_in_their_rows(dtype, rows, V, D):
+    """In each form of the logits: a row of -inf has lse -inf, one logit of +inf gives lse +inf and logp -inf elsewhere, NaN
+    gives NaN; every other row is as without them."""
+    rng = np.random.default_rng(rows)
+    ids = rng.integers(0, V, size=rows + 1).astype(np.int32)
+    ids[10] = 5
+    tok = dta.tokens_build(dta.tree_build([-1], [rows + 1]), ids, V)
+    p = dta.VocabParams(D, 1.0, KIND[dtype])
+    g = torch.Generator(device="cuda")
+    g.manual_seed(rows)
+    h = torch.randn(rows + 1, D, generator=g, device="cuda").to(TORCH[dtype])
+    w = (torch.randn(V, D, generator=g, device="cuda") * (2 / math.sqrt(D))).to(TORCH[dtype])
+    h[:, 0], w[:, 0] = 0.0, 1.0
+    logp, lse = dta.tree_logprob_fwd(tok, p, h, w)
+    w[77, 0] = 1.0e38
+    h[5, 0], h[6, 0], h[9, 0], h[rows - 1, 0] = -math.inf, math.nan, 1.0e38, math.nan
+    logp2, lse2 = dta.tree_logprob_fwd(tok, p, h, w)
+    assert float(lse2[5]) == -math.inf and math.isnan(float(lse2[6])) and float(lse2[9]) == math.inf
+    assert math.isnan(float(lse2[rows - 1])) and math.isnan(float(logp2[rows])) and float(logp2[10]) == -math.inf
+    rest = torch.ones(rows + 1, dtype=torch.bool, device="cuda")
+    rest[[5, 6, 9, rows - 1]] = False
+    # (fp32 with NaN is multiplied on the fp32 instruction: other roundings)
+    hd, wd = h[rest][:, 1:].double(), w[:, 1:].double()
+    zb = float((hd.abs() @ wd.abs().t().contiguous()).max()) * (D * UM + U)
+    lb = (128 + math.ceil(V / 128) / 64 + 12) * UM
+    bound = 0 if dtype == "bf16" else 2 * (zb + lb)
+    assert ((lse2 - lse).abs()[rest] <= bound).all()
+    after = torch.ones(rows + 1, dtype=torch.bool, device="cuda")
+    after[[6, 7, 10, rows]] = False
+    assert ((logp2 - logp).abs()[after] <= 2 * bound).all()
