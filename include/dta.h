@@ -466,8 +466,9 @@ int dta_tokens_view(const dta_tokens_t* tokens, dta_tokens_view_t* out);
 int dta_tokens_prepare(dta_tokens_t* tokens);
 
 /* Frees host and device memory.  NULL is allowed.  Does not block: the device copies are
- * released once the calls already enqueued have finished.  The tables must outlive any
- * captured graph that replays calls made on them.  Calls may be made from several host
+ * released once the calls already enqueued have finished (their streams must not be
+ * destroyed before that).  The tables must outlive any captured graph that replays calls
+ * made on them.  Calls may be made from several host
  * threads and on several streams at once, with a workspace each. */
 void dta_tokens_destroy(dta_tokens_t* tokens);
 

@@ -123,6 +123,86 @@ def test_embeddings_larger_than_the_memory_side_cache(dtype, T, V, D):
     assert (d_table[n[:, 0] == 0] == 0).all()
 
 
+@pytest.mark.parametrize("dtype,V,D", [("bf16", 300, 64), ("f32", 33, 64), ("f32", 2000, 128)])
+def test_more_rows_than_a_launch_has_blocks_for(dtype, V, D):
+    """Rows from 2^23 on are gathered (fp32, 2000 ids: split into parts) in a further round: rows on both sides of it with
+    gradients, all others without, against 64 bits."""
+    rows = 2 ** 23 + 70
+    rng = np.random.default_rng(V)
+    ids = rng.integers(0, V, size=rows + 1).astype(np.int32)
+    tok = dta.tokens_build(dta.tree_build([-1], [rows + 1]), ids, V)
+    p = dta.VocabParams(D, 1.0, KIND[dtype])
+    g = torch.Generator(device="cuda")
+    g.manual_seed(V)
+    h = torch.randn(rows + 1, D, generator=g, device="cuda", dtype=TORCH[dtype])
+    w = (torch.randn(V, D, generator=g, device="cuda") * (2 / math.sqrt(D))).to(TORCH[dtype])
+    at = np.unique(np.concatenate(([0, 2 ** 23 - 1, 2 ** 23, 2 ** 23 + 1, rows - 1], rng.integers(0, rows, size=50))))
+    t = torch.from_numpy(at).cuda()
+    d = torch.zeros(rows + 1, device="cuda")
+    d[t + 1] = torch.randn(len(at), generator=g, device="cuda")
+    logp, lse = dta.tree_logprob_fwd(tok, p, h, w)
+    d_h, d_w = dta.tree_logprob_bwd(tok, p, h, w, lse, d)
+    hd, wd = h[t].double(), w.double()
+    z = hd @ wd.t().contiguous()
+    ref = torch.logsumexp(z, 1)
+    zb = float((hd.abs() @ wd.abs().t().contiguous()).max()) * (D * UM + U)
+    lb = (128 + math.ceil(V / 128) / 64 + 12) * UM
+    assert ((lse[t].double() - ref).abs() <= zb + lb + 4 * U * ref.abs()).all()
+    n, dd = torch.arange(len(at), device="cuda"), d[t + 1].double()
+    dz = -torch.exp(z - ref[:, None]) * dd[:, None]
+    size = dz.abs()
+    of = torch.from_numpy(ids[at + 1]).cuda().long()
+    dz[n, of] += dd
+    size[n, of] += dd.abs()
+    q = 2 * zb + lb + 4 * U * ref.abs().max().item() + (2 * U if dtype == "f32" else 2.0 ** -8)
+    half = U if dtype == "f32" else 2.0 ** -8
+    for got, want, b in ((d_h[t], dz @ wd, (q + V * UM) * (size @ wd.abs())),      # (rows of zeros add nothing, exactly)
+                         (d_w, dz.t().contiguous() @ hd, (q + (len(at) + 8) * UM) * (size.t().contiguous() @ hd.abs()))):
+        over = (got.double() - want).abs() - (b + half * (want.abs() + b))
+        assert over.max().item() <= 0, over.max().item()
+    d_h[t] = 0
+    assert (d_h == 0).all()
+
+
+def test_fp32_numbers_near_the_smallest():
+    """Parts of hidden states and of the matrix around 2^-112 and 2^-120: numbers are held to 2^-134, so nothing is taken for
+    zero that bf16 can hold."""
+    V, D, rows = 20000, 512, 3000
+    rng = np.random.default_rng(9)
+    ids = rng.integers(0, V, size=rows + 1).astype(np.int32)
+    tok = dta.tokens_build(dta.tree_build([-1], [rows + 1]), ids, V)
+    p = dta.VocabParams(D, 1.0, dta.F32)
+    assert dta.vocab_workspace_bytes(tok, p, dta.VOCAB_LOGPROB_BWD) >= 6 * V * D + 6 * rows * D    # in three parts
+    g = torch.Generator(device="cuda")
+    g.manual_seed(9)
+    at, t = torch.arange(rows, device="cuda"), torch.from_numpy(ids).cuda().long()[1:]
+    d = torch.randn(rows + 1, generator=g, device="cuda")
+    for eh, ew in ((-112, 0), (0, -112), (-120, 0), (0, -120)):
+        h = torch.randn(rows + 1, D, generator=g, device="cuda") * 2.0 ** eh
+        w = torch.randn(V, D, generator=g, device="cuda") * 2.0 ** ew
+        logp, lse = dta.tree_logprob_fwd(tok, p, h, w)
+        d_h, d_w = dta.tree_logprob_bwd(tok, p, h, w, lse, d)
+        hd, wd = h[:rows].double(), w.double()
+        z = hd @ wd.t().contiguous()                      # (all but zero)
+        ref = torch.logsumexp(z, 1)
+        lb = (128 + math.ceil(V / 128) / 64 + 12) * UM + 4 * U * ref.abs().max().item()
+        assert ((lse[:rows].double() - ref).abs() <= lb).all()
+        dz = -torch.exp(z - ref[:, None]) * d[1:, None].double()
+        size = dz.abs()
+        dz[at, t] += d[1:].double()
+        size[at, t] += d[1:].double().abs()
+        del z
+        q = lb + 2 * U
+        lost = 2.0 ** -134                                # of every number of the small operand
+        for got, want, mag, n, of, least in ((d_h[:rows], dz @ wd, size @ wd.abs(), V, size.sum(1)[:, None], ew),
+                                             (d_w, dz.t().contiguous() @ hd, size.t().contiguous() @ hd.abs(), rows, size.sum(0)[:, None], eh)):
+            b = (q + n * UM) * mag + (lost * of if least else 0)
+            over = (got.double() - want).abs() - (b + U * (want.abs() + b) + 2.0 ** -149)
+            assert over.max().item() <= 0, (eh, ew, over.max().item())
+            if least:      # bounds of sums are far: by norm too, sums whose roundings vary in sign, and what is lost
+                assert (got.double() - want).norm() <= 4e-6 * want.norm() + lost * of.mul(1.0).norm() * math.sqrt(D)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("rows,V,D", [(39, 300, 64), (300, 33000, 64), (1100, 16500, 64), (18700, 290, 320)])
 def test_infinite_logits_and_nan_stay_in_their_rows(dtype, rows, V, D):
@@ -155,3 +235,70 @@ def test_infinite_logits_and_nan_stay_in_their_rows(dtype, rows, V, D):
     after = torch.ones(rows + 1, dtype=torch.bool, device="cuda")
     after[[6, 7, 10, rows]] = False
     assert ((logp2 - logp).abs()[after] <= 2 * bound).all()
+
+
+@pytest.mark.parametrize("rows,V,D", [(39, 300, 64), (300, 33000, 64), (1100, 16500, 64), (18700, 290, 320)])
+def test_gradients_of_other_rows_do_not_see_nan(rows, V, D):
+    """d_hidden of a row is its own: NaN in two hidden rows changes no bit of the others'."""
+    rng = np.random.default_rng(rows)
+    tok = dta.tokens_build(dta.tree_build([-1], [rows + 1]), rng.integers(0, V, size=rows + 1).astype(np.int32), V)
+    p = dta.VocabParams(D, 1.0, dta.BF16)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(rows)
+    h = torch.randn(rows + 1, D, generator=g, device="cuda").bfloat16()
+    w = (torch.randn(V, D, generator=g, device="cuda") * (2 / math.sqrt(D))).bfloat16()
+    d = torch.randn(rows + 1, generator=g, device="cuda")
+    _, lse = dta.tree_logprob_fwd(tok, p, h, w)
+    want, _ = dta.tree_logprob_bwd(tok, p, h, w, lse, d, want_weight=False)
+    bad = [6, rows - 1]
+    h[bad, 3] = math.nan
+    _, lse = dta.tree_logprob_fwd(tok, p, h, w)
+    got, d_w = dta.tree_logprob_bwd(tok, p, h, w, lse, d)
+    assert bool(torch.isnan(got[bad]).all()) and bool(torch.isnan(d_w).all())
+    want[bad] = got[bad] = 0
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dtype,rows,V,D", [("f32", 3000, 20000, 512), ("bf16", 100, 5000, 320), ("bf16", 600, 5000, 320),
+                                            ("f32", 30, 700, 128)])
+def test_two_graphs_of_the_same_tables(dtype, rows, V, D):
+    """A step that adds both gradients of a tied matrix, captured twice and replayed in turn on inputs that change: fp32 with
+    and without a number too large for three parts (the device finds out which, in every replay)."""
+    rng = np.random.default_rng(rows)
+    tok = dta.tokens_build(dta.tree_build([-1, 0, 0], [rows - 10, 7, 5]), rng.integers(0, V, size=rows + 2).astype(np.int32), V)
+    tok.prepare()
+    p = dta.VocabParams(D, 1.0, KIND[dtype])
+    g = torch.Generator(device="cuda")
+    g.manual_seed(rows)
+    T = rows + 2
+    h0 = torch.randn(T, D, generator=g, device="cuda").to(TORCH[dtype])
+    h, d_x = h0.clone(), torch.randn(T, D, generator=g, device="cuda").to(TORCH[dtype])
+    w = (torch.randn(V, D, generator=g, device="cuda") * (2 / math.sqrt(D))).to(TORCH[dtype])
+    w[:, 0] = 0.0
+    d = torch.randn(T, generator=g, device="cuda")
+
+    def step():
+        acc = torch.ones(V, D, device="cuda")
+        logp, lse = dta.tree_logprob_fwd(tok, p, h, w)
+        d_h, _ = dta.tree_logprob_bwd(tok, p, h, w, lse, d, None, acc, add=True)
+        return logp, lse, d_h, dta.tree_embed_bwd(tok, p, d_x, acc, add=True)
+
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        step()
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for _ in range(2):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=s):
+            outs.append(step())
+    for k in range(6):
+        h.copy_(torch.roll(h0, k, 0))
+        if k % 3 == 1:
+            h[rows // 2, 0] = 2.0 ** 41
+        graphs[k % 2].replay()
+        torch.cuda.synchronize()
+        held = [t.clone() for t in outs[k % 2]]
+        for a, b in zip(held, step()):
+            assert bool(torch.isfinite(a).all()) and torch.equal(a, b), k
+        torch.cuda.synchronize()
